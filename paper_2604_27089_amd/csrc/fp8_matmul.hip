@@ -63,7 +63,18 @@ __device__ __forceinline__ void multiply_in_place(f32x4& acc, const i32x8& a, co
 __device__ __forceinline__ void clear_in_place(f32x4& acc, const u32x2& zeros) {
     asm volatile(SP_MFMA_PRE "v_mfma_f32_4x4x4_16b_bf16 %0, %1, %1, 0" SP_MFMA_POST : "+a"(acc) : "v"(zeros));
 }
-__device__ __forceinline__ void matrix_results() { asm volatile("s_nop 15\n\ts_nop 7" ::: "memory"); }
+// Nothing but the accumulators themselves keeps a read of them behind the wait, so the statements behind it hand each one on, and
+// nothing is scheduled across them (without either, copies for a store's operand went in front of the wait).
+template <int NA, int NB>
+__device__ __forceinline__ void matrix_results(f32x4 (&acc)[NA][NB]) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) asm volatile("" : "+a"(acc[i][j]));
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 __device__ __forceinline__ i32x8 join(const u32x4& lo, const u32x4& hi) {
     i32x8 r;
@@ -393,7 +404,7 @@ __global__ __launch_bounds__(256, pipe_groups(GM, GN, STAGES)) void matmul_pipe_
             const uint32_t pitch = (p.N + 3) / 4 * 4;
             const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(
                 (float*)p.out + ((size_t)(tile / whole) * p.M + m0) * pitch + n0, 0, (int)(4 * (rows * pitch - n0)), kRawBuffer);
-            matrix_results();
+            matrix_results(acc);
             sp::static_for<0, GN>([&](auto h) {
                 const int c = 64 * GN * wc + 4 * lo + 64 * h;
                 const int off = n0 + c < pitch ? 4 * ((64 * GM * wr + 16 * hi) * (int)pitch + c) : (int)0x80000000;
@@ -413,7 +424,7 @@ __global__ __launch_bounds__(256, pipe_groups(GM, GN, STAGES)) void matmul_pipe_
         auto at_column = [&](int c) __attribute__((always_inline)) {
             return n0 + c < p.N ? (64 * GM * wr + 16 * hi) * pitch + 2 * c : (int)0x80000000;
         };
-        matrix_results();
+        matrix_results(acc);
         sp::static_for<0, GN>([&](auto h) {
             const int off = at_column(col + 64 * h);
             const int one[3] = {at_column(col + 64 * h + 1), at_column(col + 64 * h + 2), at_column(col + 64 * h + 3)};
