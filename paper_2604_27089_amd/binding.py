@@ -155,12 +155,15 @@ def _expect(t: torch.Tensor, shape, dtype, name: str):
 
 
 def _new(stream, shape, dtype, device) -> torch.Tensor:
-    """A tensor allocated by a wrapper.  torch's allocator ties a block to the stream that was current when it
-    was allocated; when the kernels go to another stream the block is marked as in use there, so that it is
-    not handed out again while they are still queued."""
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None:
-        t.record_stream(stream)
+    """A tensor allocated by a wrapper.  torch's allocator ties a block to the stream that is current when it is allocated, and may
+    hand out one that work queued there still uses.  When the kernels go to another stream the block comes from that one, and
+    is marked as in use on the caller's, whose work may still read it when the caller lets go of it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    caller = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(caller)
     return t
 
 
