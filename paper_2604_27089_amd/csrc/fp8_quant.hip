@@ -62,16 +62,19 @@ __device__ __forceinline__ uint32_t convert8(const u32x4& x, const u32x4& w, flo
 // after that write, and drop it).
 // A wave per row took longer throughout (one row of 4096 5.7 against 3.5 us, 1031 x 5120 10.4 / 5.9, 16384 x 4096 86.7 / 82.4): a row's
 // loads are four times as deep then, and few rows leave most of the chip idle.  16384 x 4096: 470 MB at 6.0 TB/s (79 us).
+// Rows lie over two dimensions of the grid, kRowsX in the first: a launch has less than 2^32 threads in a dimension.
+constexpr int64_t kRowsX = (int64_t)1 << 22;
 template <int NVT, int THREADS, bool RES>
 __global__ __launch_bounds__(THREADS) void rmsnorm_fp8_kernel(const __bf16* x, const __bf16* res, const __bf16* __restrict__ w,
                                                              __bf16* h, uint8_t* __restrict__ q, uint8_t* __restrict__ q_scale,
                                                              float* __restrict__ rstd, int64_t T, int32_t C, int64_t scale_pitch,
                                                              float eps) {
     __shared__ float sums[THREADS / 64];
-    const int64_t row = blockIdx.x;
+    const int64_t row = blockIdx.x + blockIdx.y * kRowsX;
     const int32_t Cp = (C + kBlock - 1) / kBlock * kBlock;
     if (row >= T) {  // entries behind the last row, up to a multiple of 16
-        for (int b = threadIdx.x; b < Cp / kBlock; b += THREADS) q_scale[b * scale_pitch + row] = 1;
+        if (row < scale_pitch)
+            for (int b = threadIdx.x; b < Cp / kBlock; b += THREADS) q_scale[b * scale_pitch + row] = 1;
         return;
     }
     u32x4 xv[NVT], wv[NVT];
@@ -301,7 +304,8 @@ sp_status launch_rmsnorm_fp8_fwd(const void* x, const void* res, const void* w, 
                                  int64_t T, int32_t C, float eps, hipStream_t st) {
     const int64_t pitch = up(T, 16);
     const int vectors = (int)(up(C, kBlock) / 8);
-#define SP_NORM_(NVT, N, RES) hipLaunchKernelGGL((rmsnorm_fp8_kernel<NVT, N, RES>), dim3((unsigned)pitch), dim3(N), 0, st, (const __bf16*)x, (const __bf16*)res, (const __bf16*)w, (__bf16*)h, (uint8_t*)q, (uint8_t*)q_scale, rstd, T, C, pitch, eps)
+    const dim3 grid((unsigned)(pitch < kRowsX ? pitch : kRowsX), (unsigned)((pitch + kRowsX - 1) / kRowsX));
+#define SP_NORM_(NVT, N, RES) hipLaunchKernelGGL((rmsnorm_fp8_kernel<NVT, N, RES>), grid, dim3(N), 0, st, (const __bf16*)x, (const __bf16*)res, (const __bf16*)w, (__bf16*)h, (uint8_t*)q, (uint8_t*)q_scale, rstd, T, C, pitch, eps)
 #define SP_NORM(NVT, N) do { if (res) SP_NORM_(NVT, N, true); else SP_NORM_(NVT, N, false); } while (0)
     // two vectors per thread at most: 16384 x 8192 with 512 threads 163 us, with 256 164 (64 x 8192 4.3 / 4.8); 16384 x 4096 with 256 82,
     // with 512 83, with 128 84.  No more waves than the row fills: 16384 x 5120 without a residual with 320 threads 50, with 512 56;
