@@ -361,11 +361,13 @@ sp_status sp_swiglu_bwd(const void* g, const void* u, const void* dy, void* dg, 
  *     (q, q_scale)   = operand of v    [T, C]: products that contract over C
  *     (qt, qt_scale) = operand of v^T  [C, T]: products that contract over T, as a
  *                      weight gradient's
- *   Either pair may be NULL.  C % 8 == 0 (SP_ERR_UNSUPPORTED otherwise).
+ *   Either pair may be NULL.  C % 8 == 0 (SP_ERR_UNSUPPORTED otherwise); less than 2^24
+ *   blocks of 128 x 128 (SP_ERR_SHAPE).
  *
  * sp_fp8_matmul: out[m, n] (+)= sum_k a[m, k] * b[n, k] over operands a [M, K] of
  *   type a_type and b [N, K], e4m3, with K the padded extent (K % 128 == 0,
- *   SP_ERR_UNSUPPORTED otherwise); N and K at most 2^22, M below 2^31.  out [M, N] is
+ *   SP_ERR_UNSUPPORTED otherwise); N and K at most 2^22, M below 2^31, and results in
+ *   fp32 less than 2^24 blocks of 128 x 128 (SP_ERR_SHAPE otherwise).  out [M, N] is
  *   SP_OUT_BF16 or SP_OUT_F32; accumulate != 0 adds to what out holds (fp32 only).
  *   SP_OUT_F32: products exact, sums in fp32; an operand's values have bf16's range
  *   here (from 2^128 on infinite, below 2^-133 zero).  SP_OUT_BF16: the matrix instruction

@@ -660,10 +660,12 @@ __global__ __launch_bounds__(64 * WAVES) void matmul_few_kernel(MatmulArgs p, ui
 using namespace sp::ways;
 
 template <int WAY, bool E5M2, bool F32>
-void launch_few(const MatmulArgs& p, hipStream_t st) {
+bool launch_few(const MatmulArgs& p, hipStream_t st) {
     const FewGrid g = few_grid(WAY, p.M, p.N);
+    if (!sp::launchable(g.x, 64 * kFewWaves[WAY])) return false;
     hipLaunchKernelGGL((matmul_few_kernel<kFewMB[WAY], kFewNB[WAY], kFewWaves[WAY], kFewStages[WAY], E5M2, F32>), dim3((unsigned)g.x, (unsigned)g.y),
                        dim3(64 * kFewWaves[WAY]), 0, st, p, (uint32_t)g.groups);
+    return true;
 }
 template <int WAY, bool E5M2>
 bool launch_pipe(const MatmulArgs& p, hipStream_t st) {
@@ -685,15 +687,15 @@ void launch_split(MatmulArgs p, const Split& s, float* sums, hipStream_t st) {
 }
 template <bool E5M2, bool F32>
 bool launch_way(int way, const MatmulArgs& p, hipStream_t st) {
-    if (way == 0) return launch_few<0, E5M2, F32>(p, st), true;
-    if (way == 1) return launch_few<1, E5M2, F32>(p, st), true;
-    if (way == 2) return launch_few<2, E5M2, F32>(p, st), true;
-    if (way == 3) return launch_few<3, E5M2, F32>(p, st), true;
-    if (way == 4) return launch_few<4, E5M2, F32>(p, st), true;
-    if (way == 5) return launch_few<5, E5M2, F32>(p, st), true;
+    if (way == 0) return launch_few<0, E5M2, F32>(p, st);
+    if (way == 1) return launch_few<1, E5M2, F32>(p, st);
+    if (way == 2) return launch_few<2, E5M2, F32>(p, st);
+    if (way == 3) return launch_few<3, E5M2, F32>(p, st);
+    if (way == 4) return launch_few<4, E5M2, F32>(p, st);
+    if (way == 5) return launch_few<5, E5M2, F32>(p, st);
     if constexpr (F32) {
         const int64_t mt = parts(p.M, 128), nt = parts(p.N, 128);
-        if (mt * nt > 0x7fffffff) return false;
+        if (!sp::launchable(mt * nt, 256)) return false;
         hipLaunchKernelGGL((matmul_f32_kernel<E5M2>), dim3((unsigned)(mt * nt)), dim3(256), 0, st, p, (uint32_t)mt, (uint32_t)nt);
         return true;
     } else {
@@ -728,6 +730,18 @@ sp_status launch_fp8_matmul(const void* a, const void* a_scale, const void* b, c
     const MatmulArgs p{(const uint8_t*)a, (const uint8_t*)a_scale, (const uint8_t*)b, (const uint8_t*)b_scale, out,
                        (uint32_t)M, (uint32_t)N, (uint32_t)K, (uint32_t)((M + 15) / 16 * 16), (uint32_t)((N + 15) / 16 * 16), accumulate};
     const int way = which_way(M, N, K, f32);
+    if (K == 0) {  // nothing is read: nothing is added, or zeros by as many launches as the rows need
+        if (accumulate) return SP_OK;
+        constexpr int64_t kMost = (int64_t)1 << 26;
+        bool fits = true;
+        for (int64_t m = 0; m < M && fits; m += kMost) {
+            MatmulArgs part = p;
+            part.out = (char*)out + (size_t)m * (size_t)N * (f32 ? 4 : 2);
+            part.M = (uint32_t)(M - m < kMost ? M - m : kMost);
+            fits = f32 ? launch_way<false, true>(way, part, st) : launch_way<false, false>(way, part, st);
+        }
+        return fits ? launch_status() : SP_ERR_SHAPE;
+    }
     const bool fits = a_e5m2 ? (f32 ? launch_way<true, true>(way, p, st) : launch_way<true, false>(way, p, st))
                              : (f32 ? launch_way<false, true>(way, p, st) : launch_way<false, false>(way, p, st));
     return fits ? launch_status() : SP_ERR_SHAPE;

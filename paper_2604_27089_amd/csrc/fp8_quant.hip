@@ -320,7 +320,7 @@ sp_status launch_rmsnorm_fp8_fwd(const void* x, const void* res, const void* w, 
 sp_status launch_fp8_quant(const void* x, const float* rstd, const void* w, void* q, void* q_scale, void* qt, void* qt_scale,
                            int64_t T, int32_t C, bool e5m2, hipStream_t st) {
     const int64_t cbs = up(C, kBlock) / kBlock, tiles = cbs * (up(T, kBlock) / kBlock);
-    if (tiles > 0x7fffffff) return SP_ERR_SHAPE;
+    if (!launchable(tiles, 256)) return SP_ERR_SHAPE;
     const dim3 grid((unsigned)tiles), block(256);
 #define SP_QUANT_(R, CO, N, E) hipLaunchKernelGGL((quant_kernel<R, CO, N, E>), grid, block, 0, st, (const __bf16*)x, rstd, (const __bf16*)w, (uint8_t*)q, (uint8_t*)q_scale, (uint8_t*)qt, (uint8_t*)qt_scale, T, C, up(T, 16), up(C, 16), (int32_t)cbs)
 #define SP_QUANT(R, CO) do { if (w) { if (e5m2) SP_QUANT_(R, CO, true, true); else SP_QUANT_(R, CO, true, false); } \

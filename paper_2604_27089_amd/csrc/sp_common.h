@@ -13,6 +13,8 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 inline sp_status launch_status() {
     return hipGetLastError() == hipSuccess ? SP_OK : SP_ERR_LAUNCH;
 }
+// A launch holds less than 2^32 threads in a dimension.  Beyond that the runtime runs a part of them and reports no error.
+inline bool launchable(int64_t blocks, int64_t threads) { return blocks < ((int64_t)1 << 32) / threads; }
 
 // Where row r (0 <= r < S) of an attention-side [S, H, D] tensor lives, in elements from the start of
 // its batch entry (the head offset h*D comes on top).  Two layouts are served by the same kernels:

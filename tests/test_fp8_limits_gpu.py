@@ -28,3 +28,14 @@ def test_norm_of_more_rows_than_one_launch_dimension_holds(T, C, res):
         assert torch.equal(qs[:, part].view(torch.uint8), qs2[:, :16].view(torch.uint8)) and torch.equal(rstd[part], rstd2), at
         _, y, _ = rf.norm_fwd(host_f64(h2), None, host_f64(w), EPS, None)
         check_norm_operand(q2, qs2, y, f"rows from {at}")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,N", [((1 << 27) + 5, 1), ((1 << 26) + 1, 3)])
+def test_product_without_contraction_of_many_rows(M, N, dtype):
+    """16 rows a workgroup of 512 threads: 2^27 rows are 2^32 threads."""
+    z = lambda R: torch.empty((R, 0), dtype=torch.float8_e4m3fn, device="cuda")  # noqa: E731
+    e = lambda R: torch.empty((0, (R + 15) // 16 * 16), dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)  # noqa: E731
+    out = torch.full((M, N), 7.0, device="cuda", dtype=dtype)
+    sp.sp_fp8_matmul(z(M), e(M), z(N), e(N), out=out)
+    assert not out.any()
