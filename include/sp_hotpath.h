@@ -24,6 +24,9 @@
  *   - Errors are return codes.  Argument errors are found before any launch
  *     (no GPU is needed to get them); a failed launch gives SP_ERR_LAUNCH.
  *   - Empty problems (a zero extent) return SP_OK without launching.
+ *   - A problem of so many elements that a launch would hold 2^32 threads in one
+ *     dimension (from 2^26 rows of a norm or 2^35 elements of a gate on) gives
+ *     SP_ERR_SHAPE.
  *   - No global mutable state (sp_attn_varlen_fwd_static excepted, see there):
  *     calls from several host threads are safe as long as they do not share
  *     output or workspace buffers.

@@ -121,7 +121,7 @@ sp_status launch(const AttnArgs& a, hipStream_t st) {
     if (a.stages & SP_BWD_STAGE_DELTA) {
         const int64_t lanes = (int64_t)a.B * a.S_pad * a.Hq * (D / 8);
         const int64_t blocks = (lanes + 255) / 256;
-        if (blocks > 0x7fffffff) return SP_ERR_SHAPE;
+        if (!launchable(blocks, 256)) return SP_ERR_SHAPE;
         hipLaunchKernelGGL((delta_kernel<D>), dim3((unsigned)blocks), dim3(256), 0, st, (const __bf16*)a.o,
                            (const __bf16*)a.dO, a.lse, a.delta, a.aux, a.B, a.S, a.S_pad, a.Hq,
                            1.0f / a.scale, a.qmap);
@@ -136,7 +136,7 @@ sp_status launch(const AttnArgs& a, hipStream_t st) {
     if ((a.stages & SP_BWD_STAGE_DKDV) && a.chunks.nsplit > 1) {
         const int32_t tiles = order_tiles(a.Skv);
         const int64_t blocks = (int64_t)a.B * a.Hkv * tiles * (kOrderTile / 4 / (256 / (D / 2)));
-        if (blocks > 0x7fffffff) return SP_ERR_SHAPE;
+        if (!launchable(blocks, 256)) return SP_ERR_SHAPE;
         hipLaunchKernelGGL((dkdv_reduce_kernel<D>), dim3((unsigned)blocks), dim3(256), 0, st, a.dkdv_part, (__bf16*)a.dk,
                            (__bf16*)a.dv, a.chunks, tiles, a.scale, a.kvmap, a.S, a.Skv, a.off, a.Hq / a.Hkv, a.Hkv,
                            (int64_t)a.B * a.Hkv);

@@ -445,7 +445,7 @@ sp_status launch_groups(const AttnArgs& a, hipStream_t st) {
 namespace sp {
 
 sp_status launch_attn_fwd(const AttnArgs& a, hipStream_t st) {
-    if ((int64_t)a.B * a.Hq > 0x7fffffff) return SP_ERR_SHAPE;
+    if (!launchable((int64_t)a.B * a.Hq, kThreads)) return SP_ERR_SHAPE;
     const bool varlen = a.row_lo != nullptr;
     if (a.D == 128) return varlen ? launch_groups<128, true>(a, st) : launch_groups<128, false>(a, st);
     if (a.D == 64) return varlen ? launch_groups<64, true>(a, st) : launch_groups<64, false>(a, st);

@@ -62,7 +62,7 @@ sp_status launch_attn_merge(float* o_acc, float* lse_acc, const void* o_blk, con
                             int64_t B, int64_t S, int32_t Hq, int32_t D, hipStream_t st) {
     const int64_t n_vec = B * S * Hq;
     const int64_t blocks = (n_vec * (D / 4) + 255) / 256;
-    if (blocks > 0x7fffffff) return SP_ERR_SHAPE;
+    if (!launchable(blocks, 256)) return SP_ERR_SHAPE;
     if (D == 128)
         hipLaunchKernelGGL((attn_merge_kernel<128>), dim3((unsigned)blocks), dim3(256), 0, st, o_acc, lse_acc,
                            (const __bf16*)o_blk, lse_blk, (__bf16*)o_out, n_vec, (int32_t)S, Hq);

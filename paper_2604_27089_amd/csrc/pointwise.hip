@@ -396,6 +396,7 @@ int32_t rmsnorm_bwd_groups(int64_t T) { return (int32_t)(T < kRmsBwdGroups ? (T 
 
 sp_status launch_rmsnorm_fwd(const void* x, const void* w, void* y, float* rstd, int64_t T, int32_t C, float eps,
                              hipStream_t st) {
+    if (!launchable((T + 3) / 4, 256)) return SP_ERR_SHAPE;
     const dim3 grid(blocks_for(T, 4)), block(256);
     const int nv = (C + 511) / 512;
 #define SP_RMS_FWD(NV) hipLaunchKernelGGL((rmsnorm_fwd_kernel<NV>), grid, block, 0, st, (const __bf16*)x, (const __bf16*)w, (__bf16*)y, rstd, T, C, eps)
@@ -431,7 +432,7 @@ sp_status launch_rmsnorm_bwd(const void* x, const void* w, const float* rstd, co
 sp_status launch_rope(const void* x, const float* cs, const float* sn, void* out, int64_t T, int32_t H, int32_t D,
                       bool conjugate, hipStream_t st) {
     const int64_t n_vec = T * H * (D / 16);
-    if ((n_vec + 255) / 256 > 0x7fffffff) return SP_ERR_SHAPE;
+    if (!launchable((n_vec + 255) / 256, 256)) return SP_ERR_SHAPE;
     hipLaunchKernelGGL(rope_kernel, dim3(blocks_for(n_vec, 256)), dim3(256), 0, st, (const __bf16*)x, cs, sn, (__bf16*)out,
                        n_vec, H, D, conjugate ? -1.0f : 1.0f);
     return launch_status();
@@ -439,7 +440,7 @@ sp_status launch_rope(const void* x, const float* cs, const float* sn, void* out
 
 sp_status launch_swiglu_fwd(const void* g, const void* u, void* y, int64_t n, hipStream_t st) {
     const int64_t n_vec = n / 8;
-    if ((n_vec + 255) / 256 > 0x7fffffff) return SP_ERR_SHAPE;
+    if (!launchable((n_vec + 255) / 256, 256)) return SP_ERR_SHAPE;
     hipLaunchKernelGGL(swiglu_fwd_kernel, dim3(blocks_for(n_vec, 256)), dim3(256), 0, st, (const __bf16*)g, (const __bf16*)u,
                        (__bf16*)y, n_vec);
     return launch_status();
@@ -447,7 +448,7 @@ sp_status launch_swiglu_fwd(const void* g, const void* u, void* y, int64_t n, hi
 
 sp_status launch_swiglu_bwd(const void* g, const void* u, const void* dy, void* dg, void* du, int64_t n, hipStream_t st) {
     const int64_t n_vec = n / 8;
-    if ((n_vec + 255) / 256 > 0x7fffffff) return SP_ERR_SHAPE;
+    if (!launchable((n_vec + 255) / 256, 256)) return SP_ERR_SHAPE;
     hipLaunchKernelGGL(swiglu_bwd_kernel, dim3(blocks_for(n_vec, 256)), dim3(256), 0, st, (const __bf16*)g, (const __bf16*)u,
                        (const __bf16*)dy, (__bf16*)dg, (__bf16*)du, n_vec);
     return launch_status();

@@ -142,7 +142,7 @@ sp_status launch_relayout(const void* in, void* out, int64_t B, int64_t S_l, int
     const uint64_t per_block = (uint64_t)kThreads * kUnroll;
     const uint64_t blocks = (n_vec + per_block - 1) / per_block;
     if (blocks == 0) return SP_OK;
-    if (blocks > 0x7fffffffull || run > 0xffffffffull) return SP_ERR_SHAPE;
+    if (blocks > 0x7fffffffull || !launchable((int64_t)blocks, kThreads) || run > 0xffffffffull) return SP_ERR_SHAPE;
     if ((uint64_t)S_l > 0xffffffffull) return SP_ERR_SHAPE;
     const uint64_t slab = (uint64_t)S_l * run;  // vectors of one (batch, peer) slab
     if ((run & (run - 1)) == 0 && slab * (uint64_t)P + 4096 < 0xffffffffull && P <= 65535 && B <= 65535) {
@@ -158,7 +158,7 @@ sp_status launch_relayout(const void* in, void* out, int64_t B, int64_t S_l, int
             return launch_status();
         }
         const uint64_t chunks = (slab + pb - 1) / pb;
-        if (chunks * (uint64_t)P <= 0x7fffffffull) {
+        if (launchable((int64_t)(chunks * (uint64_t)P), kFastThreads)) {
             dim3 g2((unsigned)(chunks * (uint64_t)P), (unsigned)B);
 #define SP_FAST(TH, U)                                                                                   \
     hipLaunchKernelGGL((relayout_pow2_kernel<TH, U>), g2, dim3(kFastThreads), 0, st, (const u32x4*)in,    \

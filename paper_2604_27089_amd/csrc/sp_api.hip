@@ -463,7 +463,6 @@ sp_status sp_rmsnorm_fwd(const void* x, const void* w, void* y, float* rstd, int
     if (T == 0 || C == 0) return SP_OK;
     if (!x || !w || !y || !rstd) return SP_ERR_NULL;
     if (!sp::aligned16(x) || !sp::aligned16(w) || !sp::aligned16(y) || !sp::aligned16(rstd)) return SP_ERR_ALIGN;
-    if ((T + 3) / 4 > 0x7fffffff) return SP_ERR_SHAPE;
     return sp::launch_rmsnorm_fwd(x, w, y, rstd, T, C, eps, (hipStream_t)hip_stream);
 }
 
