@@ -40,3 +40,11 @@ def test_attention():
     assert L.sp_attn_fwd(*[A(i) for i in range(1, 6)], B, 1, Hq, Hq, 64, 0.125, None) == sp.SP_ERR_SHAPE
     assert L.sp_attn_merge(*[A(i) for i in range(1, 6)], 1, 1 << 20, 1 << 8, 64, None) == sp.SP_ERR_SHAPE
     assert L.sp_attn_merge(*[A(i) for i in range(1, 6)], 1, 1 << 20, 1 << 7, 128, None) == sp.SP_ERR_SHAPE
+
+
+def test_product_past_its_largest_extents():
+    f, five = sp.lib().sp_fp8_matmul, [A(i) for i in range(1, 6)]
+    for M, N, K in ((4, (1 << 22) + 1, 128), (4, 4, (1 << 22) + 128), (1 << 31, 4, 128)):
+        for out_type in (0, 1):
+            assert f(*five, M, N, K, 0, out_type, 0, None) == sp.SP_ERR_SHAPE
+        assert sp.sp_fp8_matmul_workspace_bytes(M, N, K) == 0
