@@ -55,7 +55,8 @@ class Layer:
         self.C, self.Hq, self.Hkv, self.D = C, Hq, Hkv, D
         self.norm1 = (1 + 0.1 * torch.randn(C, device=device, generator=g)).to(torch.bfloat16)
         self.norm2 = (1 + 0.1 * torch.randn(C, device=device, generator=g)).to(torch.bfloat16)
-        self.dnorm1 = self.dnorm2 = None
+        # the norms' gradients, added up in fp32 over the calls (one call's arrives in bf16)
+        self.dnorm1, self.dnorm2 = (torch.zeros(C, dtype=torch.float32, device=device) if training else None for _ in range(2))
         for name, rows, cols in (("wq", Hq * D, C), ("wk", Hkv * D, C), ("wv", Hkv * D, C), ("wo", C, Hq * D),
                                  ("wg", F, C), ("wu", F, C), ("wd", C, F)):
             setattr(self, name, Linear(draw(rows, cols), training))
@@ -80,13 +81,14 @@ class Layer:
         return self.wd.forward(s8, s8_scale), h2, (h1, rstd1, q, k, v, o, lse, ot, ot_scale, h2, rstd2, g, u, st, st_scale)
 
     def backward(self, dy, dstream, kept, cos, sin):
-        """Gradients of y and of the stream -> the gradient of x and res alike; those of the weights are added to theirs."""
+        """Gradients of y and of the stream -> the gradient of x and res alike; those of all weights are added to theirs."""
         h1, rstd1, q, k, v, o, lse, ot, ot_scale, h2, rstd2, g, u, st, st_scale = kept
         T = dy.shape[0]
         dg, du = sp.sp_swiglu_bwd(g, u, self.wd.backward(dy, st, st_scale))
         _, _, nt, nt_scale = sp.sp_fp8_quant(h2, rows=False, cols=True, rstd=rstd2, w=self.norm2)
         dn = self.wg.backward(dg, nt, nt_scale).add_(self.wu.backward(du, nt, nt_scale))
-        dh, self.dnorm2 = sp.sp_rmsnorm_res_bwd(h2, self.norm2, rstd2, dn, dstream)
+        dh, dw = sp.sp_rmsnorm_res_bwd(h2, self.norm2, rstd2, dn, dstream)
+        self.dnorm2.add_(dw)
         do = self.wo.backward(dh, ot, ot_scale)
         dq, dk, dv = sp.sp_attn_bwd(q[None], k[None], v[None], o, lse, do.view(1, T, self.Hq, self.D))
         for t in (dq[0], dk[0]):
@@ -94,7 +96,8 @@ class Layer:
         _, _, nt, nt_scale = sp.sp_fp8_quant(h1, rows=False, cols=True, rstd=rstd1, w=self.norm1)
         dn = self.wq.backward(dq.view(T, -1), nt, nt_scale)
         dn.add_(self.wk.backward(dk.view(T, -1), nt, nt_scale)).add_(self.wv.backward(dv.view(T, -1), nt, nt_scale))
-        dh, self.dnorm1 = sp.sp_rmsnorm_res_bwd(h1, self.norm1, rstd1, dn, dh)
+        dh, dw = sp.sp_rmsnorm_res_bwd(h1, self.norm1, rstd1, dn, dh)
+        self.dnorm1.add_(dw)
         return dh
 
     def decode(self, x, res, keys, values, at, cos, sin):
