@@ -88,7 +88,7 @@ class Layer:
         _, _, nt, nt_scale = sp.sp_fp8_quant(h2, rows=False, cols=True, rstd=rstd2, w=self.norm2)
         dn = self.wg.backward(dg, nt, nt_scale).add_(self.wu.backward(du, nt, nt_scale))
         dh, dw = sp.sp_rmsnorm_res_bwd(h2, self.norm2, rstd2, dn, dstream)
-        self.dnorm2.add_(dw)
+        self.dnorm2.add_(dw.float())
         do = self.wo.backward(dh, ot, ot_scale)
         dq, dk, dv = sp.sp_attn_bwd(q[None], k[None], v[None], o, lse, do.view(1, T, self.Hq, self.D))
         for t in (dq[0], dk[0]):
@@ -97,7 +97,7 @@ class Layer:
         dn = self.wq.backward(dq.view(T, -1), nt, nt_scale)
         dn.add_(self.wk.backward(dk.view(T, -1), nt, nt_scale)).add_(self.wv.backward(dv.view(T, -1), nt, nt_scale))
         dh, dw = sp.sp_rmsnorm_res_bwd(h1, self.norm1, rstd1, dn, dh)
-        self.dnorm1.add_(dw)
+        self.dnorm1.add_(dw.float())
         return dh
 
     def decode(self, x, res, keys, values, at, cos, sin):
