@@ -1,7 +1,10 @@
 """The pipelines of the block-scaled product change their accumulators by assembly MFMAs, which the compiler does not know as matrix
 instructions: it places no wait between one and a read of its result.  matrix_results() is that wait.  The compiler's own output is
 read here: on no way through a pipeline does an instruction other than an MFMA touch an accumulator that an MFMA has changed since
-the last such wait."""
+the last such wait.
+
+The copies to LDS are assembly as well, and use m0 and scalar registers in ways that the compiler does not know of: it must have
+no use of m0 of its own, and no vector instruction may write a copy's scalar registers less than five instructions in front of it."""
 import os
 import re
 import shutil
@@ -79,7 +82,7 @@ def kernels(tmp_path_factory):
     assert r.returncode == 0, r.stderr[-2000:]
     found, name = {}, None
     for line in out.read_text().split("\n"):
-        m = re.match(r"^(_Z\w*matmul_pipe_kernel\w*):", line)
+        m = re.match(r"^(_Z\w*matmul_\w*_kernel\w*):", line)
         if m:
             name = m.group(1)
             found[name] = []
@@ -91,8 +94,29 @@ def kernels(tmp_path_factory):
 
 
 def test_results_are_read_behind_their_wait(kernels):
-    assert len(kernels) == 8  # three tiles and the shared-out contraction, for two types each
-    for name, body in kernels.items():
+    pipes = {name: body for name, body in kernels.items() if "matmul_pipe_kernel" in name}
+    assert len(pipes) == 8  # three tiles and the shared-out contraction, for two types each
+    for name, body in pipes.items():
         mfmas, waits, bad = early_touches(body)
         assert mfmas >= 32 and waits == 1, (name, mfmas, waits)
         assert bad == [], f"{name}: {len(bad)} accumulators touched before their wait, first by `{bad[0]}`"
+
+
+def scalars(operand):
+    found = {int(n) for n in re.findall(r"\bs(\d+)\b", operand)}
+    for lo, hi in re.findall(r"\bs\[(\d+):(\d+)\]", operand):
+        found |= set(range(int(lo), int(hi) + 1))
+    return found
+
+
+def test_copies_have_their_registers(kernels):
+    assert len(kernels) == 34  # the pipes, few rows in six ways and fp32 tiles, for two types and (few rows) two kinds of result
+    for name, body in kernels.items():
+        lines = [s for s in (l.split(";")[0].strip() for l in body) if s and not s.startswith(".") and not s.endswith(":")]
+        copies = [i for i, s in enumerate(lines) if s.endswith(" lds") or s.startswith("global_load_lds")]
+        assert copies, name
+        for i in copies:
+            assert lines[i - 2].startswith("s_mov_b32 m0, s") and lines[i - 1] == "s_nop 0", f"{name}: {lines[i - 2:i + 1]}"
+            near = [s for s in lines[max(i - 5, 0):i] if s.startswith("v_") and scalars(s.split(",")[0]) & scalars(lines[i])]
+            assert not near, f"{name}: `{near[0]}` in front of `{lines[i]}`"
+        assert sum("m0" in re.findall(r"\bm0\b", s) for s in lines) == len(copies), f"{name}: m0 is used elsewhere"
