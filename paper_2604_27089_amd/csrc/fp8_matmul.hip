@@ -135,7 +135,7 @@ __device__ __forceinline__ i32x4 rows_from(const uint8_t* base, uint32_t row0, u
 // 1024 bytes from memory to LDS, 16 per lane from its offset plus `scalar` in the resource to `to` + 16 * lane; and 256, 4 per lane from
 // its address.  Issued as assembly: the compiler would wait for every copy under way before any read of LDS, as it cannot tell the
 // stages apart.  No register waits for a copy, so nothing is hidden from it but LDS, whose order the kernels' own waits and
-// barriers give.
+// barriers give, and what it may do to m0 and to the scalar operands just before, which a test reads from its output.
 __device__ __forceinline__ void copy_16(uint32_t to, const i32x4& from, int off, int scalar) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(from), "s"(scalar) : "memory");
 }
@@ -221,8 +221,9 @@ __device__ __forceinline__ i32x8 fragment(const uint8_t* rows, int at) {
 // What the results are added to is read under the last block's products; behind them, where all workgroups come at about the same
 // time, reads and stores took turns (28672 x 4096 x 512 297 against 208 us, 6144 x 4096 x 4096 194 / 184).
 // Bound by the conversions, a quarter of the vector unit's rate: twice the cycles of the products, on the other unit.  28672 x 4096 x
-// 16384 3000 us, 1280 TFLOP/s, what the library's product in bf16 reaches.  Waves of 128 x 64, which convert three quarters of it, were
-// slower with two workgroups of one stage (spills) and 3 to 6 % faster as a pipeline with one.
+// 16384 3110 us, 1240 TFLOP/s, where the library's product of bf16 operands, which has nothing to convert, takes 2370; 6144 x 4096 x 4096
+// 182 and 152.  Waves of 128 x 64, which convert three quarters of it, were slower with two workgroups of one stage (spills) and 3 to
+// 6 % faster as a pipeline with one workgroup a unit (6144 x 4096 x 4096 170 -> 165 us); that pipeline is not here.
 template <bool E5M2>
 __global__ __launch_bounds__(256, 2) void matmul_f32_kernel(MatmulArgs p, uint32_t mt, uint32_t nt) {
     typedef Tile<1, 1, 2, 2> T;
@@ -306,9 +307,10 @@ __global__ __launch_bounds__(256, 2) void matmul_f32_kernel(MatmulArgs p, uint32
 // A workgroup takes tiles wg, wg + gridDim.x, ... and the pipeline runs through: the copies go on with the next tile's blocks, and
 // its first fragments are in registers when the results of the last are stored.  Steps come in pairs, one for either set; an odd
 // number of blocks is filled up with one of zeros.  K > 0.
-// 16384 x 28672 x 4096 in tiles of 256 x 256: 1377 us, 2790 TFLOP/s, the library's product with one scale 1374; the matrix unit is busy
-// 0.74 of the cycles, the rest goes where the waves meet.  256 x 128 1597 us, 128 x 128 2070: 48 and 32 KB of copies for a half and a
-// quarter of the products.
+// 16384 x 28672 x 4096 in tiles of 256 x 256: 1387 us, 2780 TFLOP/s, the library's product with one scale, in turn on the same card, 1268;
+// 8192^3 347 and 339, 4096 x 6144 x 4096 84 and 86.  The matrix unit is busy 0.73 of the cycles, the rest goes where the waves meet.  Power
+// sets the clock, so the card and the operands' values do the rest: the first takes 1340 to 1430 us.  256 x 128 1597 us, 128 x 128 2070
+// (256 x 256 1336 in that run): 48 and 32 KB of copies for a half and a quarter of the products.
 // SPLIT: a tile's blocks are shared out among `splits` workgroups, `per` blocks each (the last may have fewer), whose sums go in fp32
 // to the workspace [splits][M][N rounded up to 4]; add_splits_kernel adds them in order.
 // workgroups per compute unit, by the 160 KiB of LDS

@@ -2,11 +2,12 @@
 //
 // Each way's time is estimated from its extents, and the least is taken.  A pipe workgroup takes `fixed` us, and per tile `tile` us and
 // `step` us for each block; one of the few-row kernel the same with its rounds over b's rows in place of the tiles, and with `rows` us
-// more for each block as far as its rows of a are there to be copied.  All run one workgroup per compute unit.  Nothing ends before its
-// bytes have gone through memory at 5.6 TB/s; where that takes longest the first way does, which copies least at a time.
+// more for each block as far as its rows of a are there to be copied.  All run one workgroup per compute unit.  No estimate is below the
+// time of the bytes at 5.6 TB/s and 2.5 us (fitted; single shapes come a little under it: 1 x 57344 x 8192 82 us for 86); where that takes longest
+// the first way does, which copies least at a time.
 // The constants are fitted to the times of every way over 665 shapes of 1 to 16384 rows with the layer widths of Llama models (b from
-// memory, in a graph); what the rule takes is 0.8 % slower than the best way in the mean.  Measured, us, tiles of 256 x 256 / 256 x 128 /
-// 128 x 128 / few rows with 64 x 32 at a time: 16384 x 28672 x 4096 1336 / 1597 / 2070 / -, 4096 x 6144 x 4096 97 / 89 / 115 / -, 1024 x
+// memory, in a graph, random bytes); what the rule takes is 0.8 % slower than the best way in the mean.  Measured then, us, tiles of 256 x 256
+// / 256 x 128 / 128 x 128 / few rows with 64 x 32 at a time: 16384 x 28672 x 4096 1336 / 1597 / 2070 / -, 4096 x 6144 x 4096 97 / 89 / 115 / -, 1024 x
 // 4096 x 4096 46 / 29 / 22 / 50, 128 x 4096 x 4096 46 / 25 / 21 / 12; one row, N = 4096, K = 14336: 128 x 128 57, few rows 14.  Few rows 16 x
 // 16 / 16 x 32 / 32 x 32 / 64 x 32 / 64 x 48 / 64 x 64 at a time: 16 x 4096 x 14336 14.7 / 18.3 / 22 / 29 / - / -, 16 x 57344 x 8192 93 / 90 / 92
 // / 101 / - / -, 128 x 6144 x 4096 - / - / - / 18 / 14 / 16, 128 x 8192 x 28672 - / - / - / 101 / 108 / 79.

@@ -207,7 +207,9 @@ __global__ __launch_bounds__(256) void rmsnorm_dw_kernel(const float* __restrict
 // kernels above, so the bits are theirs: a column's terms go through LDS, 64 rows at a time, to the 16 sums that take every 16th
 // row.  dx must not be dy, which the columns still read.
 // In a graph, two launches / one, us: 16 x 4096 5.6 / 4.4, 128 x 4096 7.4 / 4.3, 323 x 5120 14.2 / 7.2, 509 x 2048 10.8 / 7.2, 512 x 8192 19.1 /
-// 12.3.  With 128 columns a workgroup and a thread for each sum, 128 x 4096 6.4 and 509 x 2048 16.4: sixteen rows in flight, not all.
+// 12.3; with the tensors in the caches 16 x 4096 5.0 / 2.5, 64 x 4096 6.3 / 2.6, 512 x 4096 11.9 / 5.4, two launches at 513 x 4096 12.0.  The limit is
+// where the registers for a column's rows end.  All eight row groups are loaded whatever T is: up to 64 rows seven of them are the
+// last row again.  With 128 columns a workgroup and a thread for each sum, 128 x 4096 6.4 and 509 x 2048 16.4: sixteen rows in flight, not all.
 constexpr int64_t kResFewRows = 512;
 template <int NVT>
 __global__ __launch_bounds__(256) void rmsnorm_res_few_kernel(const __bf16* __restrict__ x, const __bf16* __restrict__ w,
